@@ -121,8 +121,10 @@ int nq_rope_backward(nq_rope r, const void* q, int64_t q_stride, const void* k, 
  *     a = scale q . k,   a = cap tanh(a / cap) where cap > 0,    out = sum p v / sum p,  p = exp(a - max a),   lse = ln sum exp a
  * over the visible keys.  A row that sees nothing gives zeros and lse = -inf.  What it does not see never reaches a row, whatever it holds
  * (NaN, infinities, memory that was never written).  Scores, statistics and sums are held in 32 bits; the probabilities are rounded to the
- * cache's type for the product with v, in two or three parts (22 bits and more for NQ_F32 results, 16 for NQ_F16 ones of an NQ_BF16 cache) where out_dtype is
- * the finer type. */
+ * cache's type for the product with v, in parts that add up: to 16 bits and more for 16-bit results, 22 and more for NQ_F32 ones.  Only calls with
+ * more than 64 rows (new tokens times q_heads / kv_heads) to a sequence on average, whose results are of the cache's type or NQ_BF16, have a single part,
+ * 8 bits of an NQ_BF16 cache, 11 of an NQ_F16 one: the results are then about as far from binary64 again as their own rounding leaves them (2-norm: 2.3e-3 instead of 1.7e-3
+ * for NQ_BF16).  Who wants those finer asks for NQ_F32 results. */
 
 /* out_dtype: of the results; q has the cache's type.  Copies what it needs of kv (which may be destroyed).  q_heads a multiple of the cache's kv_heads.  Host only. */
 int nq_attn_create(nq_attn* out, nq_kv kv, int q_heads, double scale, double cap, int out_dtype);

@@ -12,6 +12,7 @@ namespace nq {
 // How a call is cut: rows of a tile (16: attn_split_kernel; 64, 128: attn_wide_kernel) and most items of a key head
 struct AttnCut {
     int rows, slots, items;
+    bool few;                // up to 64 rows of a sequence, on average
 };
 static AttnCut cut_attention(const nq_attn_s& a, int n_seqs, int n_tokens)
 {
@@ -19,7 +20,8 @@ static AttnCut cut_attention(const nq_attn_s& a, int n_seqs, int n_tokens)
     const int group = a.q_heads / a.kv.heads;
     const int64_t rows = std::max<int64_t>(1, (int64_t)n_tokens * group / std::max(1, n_seqs));        // of a sequence, on average
     // (32 sequences of eight rows: tiles of 16 rows 130 us, of 64 137; one of 16384 rows: of 128 rows 359 us, of 64 451)
-    c.rows = rows <= 16 ? 16 : rows <= 64 || padded_dim(a.kv.head_dim) == 256 ? 64 : 128;      // (heads of 256: sums of 128 rows do not fit the registers)
+    c.few = rows <= 64;
+    c.rows = rows <= 16 ? 16 : c.few || padded_dim(a.kv.head_dim) == 256 ? 64 : 128;      // (heads of 256: sums of 128 rows do not fit the registers)
     const int to_cu = padded_dim(a.kv.head_dim) == 256 && c.rows == 16 ? 1 : 2;             // workgroups that a CU's registers hold
     c.slots = std::max(1, to_cu * device_cu_count() / a.kv.heads);
     c.items = (int)(2 * c.slots + (int64_t)n_tokens * group / c.rows + n_seqs);
@@ -117,6 +119,7 @@ extern "C" int nq_attn_forward(nq_attn a, const void* q, int64_t q_stride, const
     k.cap = a->cap;
     k.slots = c.slots;
     k.rows = c.rows;
+    k.few = c.few;
     k.items = c.items;
     const hipStream_t s = (hipStream_t)stream;
     return a->kv.dtype == NQ_F16 ? attend_f16(k, who, s) : attend_bf16(k, who, s);

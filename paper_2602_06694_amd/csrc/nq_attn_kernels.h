@@ -47,6 +47,7 @@ struct AttnArgs {
     int slots;               // workgroups of a key head that run at a time
     int items;               // most items of a key head (the grid)
     int rows;                // of a tile; 16: attn_split_kernel, 64 and 128: attn_wide_kernel
+    bool few;                // rows of a sequence, on average up to 64: bound by bytes
 };
 
 // A call, checked, over a cache of this type
@@ -518,7 +519,7 @@ __global__ __launch_bounds__(kWaves * 64, DP == 256 ? 1 : 2) void attn_split_ker
             step += kWaves;
             if (step < step1) load(step, one);
         }
-        if (PARTS == 1 || careful) break;
+        if (careful) break;
         float zero = 0.f;
 #pragma unroll
         for (int h = 0; h < kHalves; ++h)
@@ -1075,27 +1076,31 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int rows)
 
 static int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
+// PARTS: parts of the weights where there are many rows.  One part of bf16 is eight bits, an error as large as the results' own rounding: 2.3 10^-3 of the results in the 2-norm,
+// where a single rounding of exact ones leaves 1.7 10^-3.  Few rows have two parts in any case: their calls are bound by bytes for the most part (32 sequences of up to 8191:
+// 127.5 us with two parts, 127.1 with one; six tokens behind 131071: 116 and 113; five trees with capped scores, fp16 results: 60 and 53).  Many rows are bound by the matrix
+// products, and have one part where the results are of the cache's type or a coarser one: 2048 tokens behind 4095 take 341 us with one part, 454 with two.
 template <int DT, int DP, int PARTS>
 static int launch_attention(const AttnArgs& a, const char* who, hipStream_t s)
 {
+    constexpr int kFew = PARTS < 2 ? 2 : PARTS;
     const dim3 grid((unsigned)a.items * a.kv.heads), block(kWaves * 64);
     if (a.rows == 16) {
         constexpr int lds = split_lds(DP);
-        NQ_ALLOW_LDS((attn_split_kernel<DT, DP, PARTS>), lds);
-        hipLaunchKernelGGL((attn_split_kernel<DT, DP, PARTS>), grid, block, lds, s, a);
+        NQ_ALLOW_LDS((attn_split_kernel<DT, DP, kFew>), lds);
+        hipLaunchKernelGGL((attn_split_kernel<DT, DP, kFew>), grid, block, lds, s, a);
     } else {
         constexpr int lds = wide_lds(DP);
-        auto wide = [&](auto r, auto capped) {
-            constexpr int R = decltype(r)::value;
+        auto wide = [&](auto r, auto parts, auto capped) {
+            constexpr int R = decltype(r)::value, kParts = decltype(parts)::value;
             constexpr bool CAP = decltype(capped)::value;
-            NQ_ALLOW_LDS((attn_wide_kernel<DT, DP, R, PARTS, CAP>), lds);
-            hipLaunchKernelGGL((attn_wide_kernel<DT, DP, R, PARTS, CAP>), grid, block, lds, s, a);
+            NQ_ALLOW_LDS((attn_wide_kernel<DT, DP, R, kParts, CAP>), lds);
+            hipLaunchKernelGGL((attn_wide_kernel<DT, DP, R, kParts, CAP>), grid, block, lds, s, a);
             return NQ_OK;
         };
-        auto tiles = [&](auto r) { return a.cap > 0.f ? wide(r, std::true_type()) : wide(r, std::false_type()); };
-        int rc = NQ_OK;
-        if constexpr (DP < 256) rc = a.rows == 64 ? tiles(std::integral_constant<int, 1>()) : tiles(std::integral_constant<int, 2>());
-        else rc = tiles(std::integral_constant<int, 1>());
+        auto tiles = [&](auto r, auto parts) { return a.cap > 0.f ? wide(r, parts, std::true_type()) : wide(r, parts, std::false_type()); };
+        typedef std::integral_constant<int, DP < 256 ? 2 : 1> Many;          // tiles of 16 rows to a wave
+        const int rc = a.few ? tiles(std::integral_constant<int, 1>(), std::integral_constant<int, kFew>()) : tiles(Many(), std::integral_constant<int, PARTS>());
         if (rc) return rc;
     }
     if (const int rc = launched(who)) return rc;
