@@ -60,8 +60,10 @@ static int check_sizes(const char* who, nq_attn a, int n_seqs, int n_tokens)
     if (!a) return refuse(NQ_E_NULL, who, "NULL handle");
     if (n_seqs < 1) return refuse(NQ_E_INVALID_ARG, who, "n_seqs must be >= 1");
     if (n_tokens < 0) return refuse(NQ_E_INVALID_ARG, who, "n_tokens must be >= 0");
-    // rows and items are counted in 32 bits
-    if ((int64_t)n_tokens * a->q_heads > (INT64_C(1) << 30) || ((int64_t)n_seqs + 4096) * a->kv.heads > (INT64_C(1) << 30)) return refuse(NQ_E_SHAPE, who, "too many tokens or sequences for one call");
+    // rows are counted in 32 bits; a launch has fewer than 2^32 threads (and 64 sequences' items, at most one more than all to each, fit 32 bits)
+    if ((int64_t)n_tokens * a->q_heads > (INT64_C(1) << 30) || ((int64_t)n_seqs + 4096) * a->kv.heads > (INT64_C(1) << 30) ||
+        (int64_t)cut_attention(*a, n_seqs, n_tokens).items * a->kv.heads >= (INT64_C(1) << 24))
+        return refuse(NQ_E_SHAPE, who, "too many tokens or sequences for one call");
     return NQ_OK;
 }
 

@@ -86,6 +86,8 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int s)
 __device__ __forceinline__ int tiles_of(const Seq& q, const AttnArgs& a, int rows) { return (q.n * a.group + rows - 1) / rows; }
 __device__ __forceinline__ int blocks_of(const Seq& q) { return q.n > 0 ? (q.keys + kBlock - 1) / kBlock : 0; }
 __device__ __forceinline__ int runs_of(int blocks, int run) { return (blocks + run - 1) / run; }
+// items of a sequence, or one more than the call has room for: where new_begin does not rise, tiles may be more than rows, and any number of items is asked for
+__device__ __forceinline__ int items_of(int tiles, int runs, const AttnArgs& a) { return (int)min((int64_t)tiles * runs, (int64_t)a.items + 1); }
 
 // Blocks of a run, or kNoRuns.  The chip holds a.slots workgroups of a key head at a time; each would have `share` blocks if they could be dealt out evenly.  Of three
 // ways the one that is expected to end first, in blocks:
@@ -135,8 +137,8 @@ __device__ __forceinline__ bool find_item(const AttnArgs& a, int rows, int numbe
     int before = 0;
     for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
         const Seq q = s0 == 0 ? front : sequence(a, s0 + lane);
-        const int tiles = tiles_of(q, a, rows), blocks = blocks_of(q), runs = runs_of(blocks, run);
-        const int upto = before + (int)wave_scan((uint32_t)(tiles * runs));
+        const int tiles = tiles_of(q, a, rows), blocks = blocks_of(q), runs = runs_of(blocks, run), items = items_of(tiles, runs, a);
+        const int upto = before + (int)wave_scan((uint32_t)items);
         const uint64_t past = __ballot(upto > number);
         if (past) {
             const int at = __builtin_ctzll(past);
@@ -144,14 +146,16 @@ __device__ __forceinline__ bool find_item(const AttnArgs& a, int rows, int numbe
             it->q = Seq{pick(q.first), pick(q.n), pick(q.ctx), pick(q.keys)};
             it->seq = s0 + at;
             it->runs = pick(runs);
-            const int mine = number - pick(upto - tiles * runs);
+            const int first = pick(upto - items), mine = number - first;
+            // what several runs leave has to have its place, whichever of them this is (only a new_begin that does not rise has more)
+            if (it->runs > 1 && first + pick(items) > a.items) return false;
             // the tiles of a run next to one another: they read the same keys; the last first: where rows see what precedes them those have most to do, and a place
             // that is free again early then gets less than one that is free late
             const int n_tiles = pick(tiles);
             it->run = mine / n_tiles;
             it->tile = n_tiles - 1 - (mine - it->run * n_tiles);
             it->per = (pick(blocks) + it->runs - 1) / it->runs;
-            it->index = pick(upto - tiles * runs) + it->tile;
+            it->index = first + it->tile;
             return true;
         }
         before = __builtin_amdgcn_readlane(upto, 63);
@@ -954,21 +958,21 @@ __device__ __forceinline__ RowRuns find_runs(const AttnArgs& a, int rows, int ru
     for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
         const Seq q = s0 == 0 ? front : sequence(a, s0 + lane);
         const int tiles = tiles_of(q, a, rows), blocks = blocks_of(q), runs = runs_of(blocks, run);
-        const int upto = before + (int)wave_scan((uint32_t)(tiles * runs));
+        const int items = items_of(tiles, runs, a), upto = before + (int)wave_scan((uint32_t)items);
         const uint64_t here = __ballot(t >= q.first && t < q.first + q.n);
         if (here) {
             const int s = __builtin_ctzll(here);
             auto pick = [&](int v) { return __builtin_amdgcn_readlane(v, s); };
             const int n_runs = pick(runs), n_tiles = pick(tiles), n_blocks = pick(blocks);
-            const int64_t first = pick(upto - tiles * runs);
+            const int64_t first = pick(upto - items);
             const Seq mine = {pick(q.first), pick(q.n), pick(q.ctx), pick(q.keys)};
-            if (n_runs <= 1 || first + (int64_t)n_tiles * n_runs > a.items) break;               // (the latter: new_begin is no ascending list)
+            if (n_runs <= 1 || first + pick(items) > a.items) break;                                // (the latter as in find_item)
             const int row = (t - mine.first) * a.group + h % a.group, tile = row / rows;
             const int per = (n_blocks + n_runs - 1) / n_runs;
             const int used = min(n_runs, ((tile_keys(a, mine, tile, rows) + kBlock - 1) / kBlock + per - 1) / per);
             return RowRuns{used, ((first + tile) * a.kv.heads + h / a.group) * rows + (row - tile * rows), (int64_t)n_tiles * a.kv.heads * rows};
         }
-        before = __builtin_amdgcn_readlane(upto, 63);
+        before = min(__builtin_amdgcn_readlane(upto, 63), a.items + 1);
     }
     return RowRuns{0, 0, 0};
 }

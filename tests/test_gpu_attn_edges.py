@@ -23,3 +23,24 @@ def test_16_bit_results_of_few_rows_are_rounded_once(dtype, d, new, ctx):
     once = float((want.to(TORCH[dtype]).double() - want).norm())
     assert float((got.double() - want).norm()) <= 1.02 * once
     p.done()
+
+
+@pytest.mark.parametrize("begin,ctx,tokens,hq,hk", [([0, 2048] * 5, [30000] * 9, 2048, 8, 8), ([0, 320] * 7, [64] * 12 + [60000], 320, 64, 8),
+                                                    ([0, 17] * 20, [5000] * 39, 17, 8, 1)])
+def test_lists_that_do_not_rise_leave_what_is_behind_the_workspace(begin, ctx, tokens, hq, hk):
+    """More tiles than rows: what has no place in the workspace is left out.  All sequences in one page, 64 MiB of a pattern behind the workspace."""
+    d, page = 128, 16
+    begin = begin[:len(ctx) + 1]
+    k, v = (randn(i, 1, hk, page, d).to(torch.bfloat16).cuda() for i in (1, 2))
+    kv = nq.nq_kv_create(k, v, nq.NQ_BF16, hk, d, page, 1)
+    a = nq.nq_attn_create(kv, hq, 0.1, 0.0, nq.NQ_BF16)
+    need = nq.nq_attn_workspace_bytes(a, len(ctx), tokens)
+    room = torch.full((need + (64 << 20),), 0x5a, dtype=torch.uint8, device="cuda")
+    on = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    q, out = randn(3, tokens, hq * d).to(torch.bfloat16).cuda(), torch.zeros(tokens, hq * d, dtype=torch.bfloat16, device="cuda")
+    table = torch.zeros(len(ctx), (max(ctx) + tokens) // page + 1, dtype=torch.int32, device="cuda")
+    nq.nq_attn_forward(a, q, on(begin), on(ctx), table, None, out, None, room, need)
+    torch.cuda.synchronize()
+    assert bool((room[need:] == 0x5a).all())
+    nq.nq_attn_destroy(a)
+    nq.nq_kv_destroy(kv)
