@@ -163,12 +163,13 @@ __device__ __forceinline__ bool find_item(const AttnArgs& a, int rows, int numbe
     return false;
 }
 
+// keys up to a new token and its own (a length near 2^31 and a token are more than 32 bits hold)
+__device__ __forceinline__ int keys_upto(const Seq& q, int token) { return (int)min((int64_t)q.keys, (int64_t)q.ctx + token + 1); }
 // keys that some row of a tile may see: all, or up to the tile's last token where the rows see what precedes them
 __device__ __forceinline__ int tile_keys(const AttnArgs& a, const Seq& q, int tile, int rows)
 {
     if (a.tree) return q.keys;
-    const int last = min((tile + 1) * rows, q.n * a.group) - 1;
-    return (int)min((int64_t)q.keys, (int64_t)q.ctx + last / a.group + 1);
+    return keys_upto(q, (min((tile + 1) * rows, q.n * a.group) - 1) / a.group);
 }
 
 template <int DT>
@@ -666,9 +667,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_wide_kernel(AttnArgs a)
     }
     // keys that every row of the wave sees, and that some row sees
     const int last_row = min(row0 + 16 * R, all_rows) - 1;
-    const int whole = row0 >= all_rows ? 0 : a.tree ? min(it.q.keys, it.q.ctx) : min(it.q.keys, it.q.ctx + row0 / a.group + 1);
-    const int some = row0 >= all_rows ? 0 : a.tree ? it.q.keys : min(it.q.keys, it.q.ctx + last_row / a.group + 1);
-    const int tile_whole = a.tree ? min(it.q.keys, it.q.ctx) : min(it.q.keys, it.q.ctx + it.tile * kRows / a.group + 1);     // that every row of the tile sees
+    const int whole = row0 >= all_rows ? 0 : a.tree ? min(it.q.keys, it.q.ctx) : keys_upto(it.q, row0 / a.group);
+    const int some = row0 >= all_rows ? 0 : a.tree ? it.q.keys : keys_upto(it.q, last_row / a.group);
+    const int tile_whole = a.tree ? min(it.q.keys, it.q.ctx) : keys_upto(it.q, it.tile * kRows / a.group);     // that every row of the tile sees
 
     v4f o[R][kCols];
     float top[R], sum[R];                                           // (sum: of this lane's keys)

@@ -44,3 +44,30 @@ def test_lists_that_do_not_rise_leave_what_is_behind_the_workspace(begin, ctx, t
     assert bool((room[need:] == 0x5a).all())
     nq.nq_attn_destroy(a)
     nq.nq_kv_destroy(kv)
+
+
+def beyond_the_table(new, ctx, pages, tree=None, d=64, hq=4, page=16):
+    """One sequence of more tokens than its table has room for: all rows see what the table holds, once."""
+    k, v = (randn(70 + i, pages * page, 1, d).to(torch.bfloat16) for i in (1, 2))
+    kc, vc = (t.view(pages, page, 1, d).transpose(1, 2).contiguous().cuda() for t in (k, v))
+    kv = nq.nq_kv_create(kc, vc, nq.NQ_BF16, 1, d, page, pages)
+    a = nq.nq_attn_create(kv, hq, 0.125, 0.0, nq.NQ_F32)
+    n = nq.nq_attn_workspace_bytes(a, 1, new)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    on = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    q, out, lse = randn(73, new, hq * d).to(torch.bfloat16), torch.empty(new, hq * d, device="cuda"), torch.empty(new, hq, device="cuda")
+    nq.nq_attn_forward(a, q.cuda(), on([0, new]), on([ctx]), on([list(range(pages))]), tree, out, lse, ws, n)
+    torch.cuda.synchronize()
+    nq.nq_attn_destroy(a)
+    nq.nq_kv_destroy(kv)
+    want, want_lse = attention(q.double().view(new, hq, d), k.double(), v.double(), torch.ones(new, pages * page, dtype=torch.bool), 0.125)
+    # (scores of at most some 20: a weight is off by 2^-17 of itself at most, values are below 5)
+    close(out.view(new, hq, d), want, "f32", 2.0 ** -14)
+    close(lse, want_lse, "f32", 2.0 ** -16)
+
+
+@pytest.mark.parametrize("with_tree", [False, True])
+@pytest.mark.parametrize("new", [10, 40])
+def test_lengths_near_the_end_of_32_bits(new, with_tree):
+    """Tiles of 64 and of 128 rows."""
+    beyond_the_table(new, 2 ** 31 - 1, 5, torch.zeros(new, 2, dtype=torch.int32, device="cuda") if with_tree else None)
