@@ -67,7 +67,7 @@ __device__ __forceinline__ int64_t wave_sum(int64_t v)
 
 // A sequence as the device finds it, cut to the call's buffers
 struct Seq {
-    int first, n, ctx, keys;         // first new token, new tokens, cached tokens, keys in all
+    int first, n, ctx, keys;         // first new token, new tokens, cached tokens, keys in all (at least the cached ones)
 };
 __device__ __forceinline__ Seq sequence(const AttnArgs& a, int s)
 {
@@ -75,8 +75,9 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int s)
     if (s < a.n_seqs) {
         q.first = min(max(a.begin[s], 0), a.n_tokens);
         q.n = min(max(a.begin[s + 1], q.first), a.n_tokens) - q.first;
-        q.ctx = max(a.ctx[s], 0);
+        // both within the table: every key below ctx is one
         const int64_t most = min(a.table_stride << a.kv.page_shift, (int64_t)INT32_MAX - 4096);
+        q.ctx = (int)min((int64_t)max(a.ctx[s], 0), most);
         q.keys = (int)min((int64_t)q.ctx + q.n, most);
     }
     return q;

@@ -71,3 +71,11 @@ def beyond_the_table(new, ctx, pages, tree=None, d=64, hq=4, page=16):
 def test_lengths_near_the_end_of_32_bits(new, with_tree):
     """Tiles of 64 and of 128 rows."""
     beyond_the_table(new, 2 ** 31 - 1, 5, torch.zeros(new, 2, dtype=torch.int32, device="cuda") if with_tree else None)
+
+
+@pytest.mark.parametrize("new", [1, 3, 10, 40])
+@pytest.mark.parametrize("pages", [1, 3, 5, 6])
+@pytest.mark.parametrize("more", [0, 1, 15, 16, 17, 1000, 2 ** 30])
+def test_tokens_beyond_the_table_are_not_seen(new, pages, more):
+    """Tables of an odd number of pages of 16 end in the middle of a step of 32 keys."""
+    beyond_the_table(new, 16 * pages + more, pages)
