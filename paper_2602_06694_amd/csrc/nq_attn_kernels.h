@@ -983,8 +983,9 @@ __device__ __forceinline__ RowRuns find_runs(const AttnArgs& a, int rows, int ru
 struct Joined {
     v4f x = {0.f, 0.f, 0.f, 0.f};
     float total = 0.f, high = -INFINITY;
-    // of a part whose maximum is t (minus infinity: runs that the row sees nothing of)
+    // of a part whose maximum is t (minus infinity: runs that the row sees nothing of, and those of which every score is NaN, whose sum is NaN as well)
     static __device__ __forceinline__ float share(float t, float top) { return t == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(t - top); }
+    static __device__ __forceinline__ bool nothing(float t, float total) { return t == -INFINITY && total == 0.f; }
     template <int DP>
     __device__ __forceinline__ void add(const AttnArgs& a, const RowRuns& r, int d, int first, int stride)
     {
@@ -996,7 +997,7 @@ struct Joined {
                 const int64_t p = r.at + min(r0 + k * stride, r.used - 1) * r.step;
                 v[k] = d < a.kv.head_dim ? *(const v4f*)(a.part_o + p * DP + d) : v4f{0.f, 0.f, 0.f, 0.f};
                 top[k] = r0 + k * stride < r.used ? a.part_ml[p * 2] : -INFINITY;
-                sum[k] = a.part_ml[p * 2 + 1];
+                sum[k] = r0 + k * stride < r.used ? a.part_ml[p * 2 + 1] : 0.f;
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) most = fmaxf(most, top[k]);
@@ -1006,7 +1007,7 @@ struct Joined {
             high = most;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                if (top[k] == -INFINITY) continue;
+                if (nothing(top[k], sum[k])) continue;
                 const float g = share(top[k], high);
                 x += v[k] * g;
                 total += sum[k] * g;
@@ -1068,7 +1069,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int rows)
                 for (int p = 0; p < kAtOnce; ++p) sum.high = fmaxf(sum.high, lds_high[p]);
 #pragma unroll
                 for (int p = 0; p < kAtOnce; ++p) {
-                    if (lds_high[p] == -INFINITY) continue;
+                    if (Joined::nothing(lds_high[p], lds_total[p])) continue;
                     const float f = Joined::share(lds_high[p], sum.high);
                     sum.x += *(const v4f*)&lds_x[p][d] * f;
                     sum.total += lds_total[p] * f;

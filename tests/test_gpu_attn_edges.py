@@ -79,3 +79,37 @@ def test_lengths_near_the_end_of_32_bits(new, with_tree):
 def test_tokens_beyond_the_table_are_not_seen(new, pages, more):
     """Tables of an odd number of pages of 16 end in the middle of a step of 32 keys."""
     beyond_the_table(new, 16 * pages + more, pages)
+
+
+NAN_CASES = [([4000], [1], 4, 2, 128), ([9000], [3], 8, 1, 64), ([5000], [20], 4, 1, 128), ([4000], [45], 16, 2, 64), ([3000] * 40, [1] * 40, 16, 2, 64), ([6000, 10], [9, 1], 4, 2, 256)]
+
+
+def nan_problem(ctx, new, hq, hk, d):
+    """Calls whose rows are cut into runs: a row or more to a workgroup of the join, tiles of 16, 64 and 128."""
+    return Problem(81, ctx, new, hq, hk, d, "bf16", "f32", tree=[random_tree(n, 6) for n in new])
+
+
+@pytest.mark.parametrize("case", NAN_CASES)
+def test_a_query_of_nan_gives_nan(case):
+    ctx, new, hq, hk, d = case
+    p = nan_problem(*case)
+    clean, clean_lse = p.run()
+    p.q[0, d:2 * d], p.q[-1, 0] = math.nan, math.nan             # all of a head, one element of another
+    out, lse = p.run()
+    bad = torch.zeros(sum(new), hq, dtype=torch.bool)
+    bad[0, 1] = bad[-1, 0] = True
+    assert bool(torch.isnan(out[bad]).all()) and bool(torch.isnan(lse[bad]).all())
+    assert torch.equal(out[~bad], clean[~bad]) and torch.equal(lse[~bad], clean_lse[~bad])
+    p.done()
+
+
+def test_keys_of_nan_over_whole_runs_give_nan():
+    """Behind every number of blocks of 64 keys, wherever the runs end: what sees NaN is NaN."""
+    p = nan_problem([4000], [1], 4, 2, 128)
+    _, clean_lse = p.run()
+    for block in range(62, 0, -1):
+        p.k[0][64 * block:, 1] = math.nan
+        out, lse = p.run()
+        assert bool(torch.isnan(out[:, 2:]).all()) and bool(torch.isnan(lse[:, 2:]).all()), block
+        assert torch.equal(lse[:, :2], clean_lse[:, :2])
+    p.done()
