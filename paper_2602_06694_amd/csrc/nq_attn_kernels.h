@@ -485,8 +485,8 @@ __global__ __launch_bounds__(kWaves * 64, DP == 256 ? 1 : 2) void attn_split_ker
             }
     };
 
-    // With weights in parts an infinite value meets parts of both signs and zeros: where a sum is not finite the wave goes through its keys once more and takes such values
-    // out of all steps, as where they must not meet the weights of rows that do not see them.
+    // An infinite value must not meet weights that are rounded to zero, nor parts of weights of both signs: where a sum is not finite the wave goes through its keys once more and
+    // takes such values out of all steps, as where they must not meet the weights of rows that do not see them.
     for (bool careful = false;; careful = true) {
         top = -INFINITY;
         sum = 0.f;
@@ -835,7 +835,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_wide_kernel(AttnArgs a)
         add_values(buffer, weight, mend_t);
     };
 
-    // (as in attn_split_kernel: once more, if a sum is not finite and the weights are in parts; by the whole workgroup)
+    // (as in attn_split_kernel: once more, if a sum is not finite; by the whole workgroup)
     for (bool careful = false;; careful = true) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -902,7 +902,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void attn_wide_kernel(AttnArgs a)
             }
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");            // the loads past the end: nothing may arrive after the workgroup
         }
-        if (PARTS == 1 || careful) break;
+        if ((PARTS == 1 && DT == NQ_BF16) || careful) break;         // (a single part of bf16 has the range of fp32: no weight is rounded to zero)
         float zero = 0.f;
 #pragma unroll
         for (int r = 0; r < R; ++r)

@@ -113,3 +113,19 @@ def test_keys_of_nan_over_whole_runs_give_nan():
         assert bool(torch.isnan(out[:, 2:]).all()) and bool(torch.isnan(lse[:, 2:]).all()), block
         assert torch.equal(lse[:, :2], clean_lse[:, :2])
     p.done()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("new,d", [(1, 64), (40, 128), (100, 64), (100, 256)])
+def test_an_infinite_value_of_a_small_weight(dtype, new, d):
+    """exp(-60) of the largest weight is no number of fp16, but it is not zero: infinite values give infinities, one part of the weights or several."""
+    p = Problem(91, [700], [new], 4, 1, d, dtype, dtype, tree=[random_tree(new, 7)])
+    p.scale = 0.125
+    p.q.view(new, 4, d)[..., 0] = 8.0
+    p.k[0][:, 0, 0] = 0.0
+    p.k[0][[20, 300], 0, 0] = -60.0
+    p.v[0][20, 0, 5], p.v[0][300, 0, 9] = math.inf, -math.inf
+    out, lse = p.run()
+    assert bool((out[..., 5] == math.inf).all()) and bool((out[..., 9] == -math.inf).all())
+    assert int((~torch.isfinite(out)).sum()) == 2 * new * 4 and bool(torch.isfinite(lse).all())
+    p.done()
