@@ -602,11 +602,15 @@ constexpr int wide_buffers(int dp) { return dp == 256 ? 2 : 4; }           // a 
 constexpr int wide_lds(int dp) { return wide_buffers(dp) * 2 * wide_keys(dp) * dp * 2 + kWaves * (int)sizeof(int); }
 
 // 16 bytes of each lane at base + offset -> LDS, one lane's after the other's, from byte `to` on (the same in all lanes)
-// (the waits: one instruction between m0's write and its use, five between a scalar register's by the vector unit and its use as an address)
+// (the waits: one instruction between m0's write and its use, five between a scalar register's by the vector unit and its use as an address; m0 is named as written: the compiler
+// sets it before uses of its own, but may set it once for several, and warns of any reserved register in such a list)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void lds_load(const void* base, uint32_t offset, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // the order of a region with the products of a block's keys and the weights of another: an exponential and what belongs to it to every product
 template <int R, int TILES, int PARTS>
