@@ -527,6 +527,11 @@ def _rows(t, n_tokens: int, what: str):
     return t.data_ptr(), (stride[0] if n_tokens > 1 else width), width
 
 
+def _extent(t) -> int:
+    """Elements from a tensor's first to its last."""
+    return 1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())) if t.numel() else 0
+
+
 _WIDTHS = {}            # handle of a cache, rope or attention -> widths and types that the tensors of a call have to match
 _TORCH_TYPES = {}
 
@@ -560,18 +565,28 @@ def _same_length(n: int, what: str, *tensors) -> None:
 
 def nq_kv_create(k, v, dtype: int, kv_heads: int, head_dim: int, page_size: int, n_pages: int, page_stride: int = 0, slot_stride: int = 0,
                  head_stride: int = 0) -> int:
-    """k, v: device tensors (or addresses) that hold the pages; strides in elements, 0, 0, 0: [n_pages][kv_heads][page_size][head_dim]."""
+    """k, v: device tensors (or addresses) that hold the pages; strides in elements, 0, 0, 0: [n_pages][kv_heads][page_size][head_dim], for which tensors have to be
+    contiguous.  Tensors have to hold all pages."""
     h = ctypes.c_void_p()
-    at = []
+    at, tensors = [], []
     for t in (k, v):
         if t is not None and not isinstance(t, int):
             if t.dtype != _torch_type(dtype):
                 raise ValueError(f"k, v: expected {_torch_type(dtype)}, got {t.dtype}")
             if not t.is_cuda:
                 raise ValueError("k, v: expected device (cuda) tensors")
+            tensors.append(t)
             t = t.data_ptr()
         at.append(t)
     _check(lib().nq_kv_create(ctypes.byref(h), at[0], at[1], dtype, kv_heads, head_dim, page_size, n_pages, page_stride, slot_stride, head_stride))
+    packed = not (page_stride or slot_stride or head_stride)
+    need = n_pages * kv_heads * page_size * head_dim if packed else \
+        (n_pages - 1) * page_stride + (page_size - 1) * slot_stride + (kv_heads - 1) * head_stride + head_dim
+    for t in tensors:
+        whole = t.is_contiguous()
+        if need > (t.numel() if whole else _extent(t)) or (packed and not whole):
+            lib().nq_kv_destroy(h)
+            raise ValueError(f"k, v: the pages take {need} elements, {tuple(t.shape)} of strides {t.stride()} are no room for them")
     _WIDTHS[h.value] = (head_dim, _torch_type(dtype))
     return h.value
 
