@@ -129,7 +129,7 @@ int nq_rope_backward(nq_rope r, const void* q, int64_t q_stride, const void* k, 
 /* out_dtype: of the results; q has the cache's type.  Copies what it needs of kv (which may be destroyed).  q_heads a multiple of the cache's kv_heads.  Host only. */
 int nq_attn_create(nq_attn* out, nq_kv kv, int q_heads, double scale, double cap, int out_dtype);
 int nq_attn_destroy(nq_attn a);
-/* Workspace of a call with n_seqs sequences and n_tokens new tokens in all. */
+/* Workspace of a call with n_seqs sequences and n_tokens new tokens in all; it serves every call with fewer of either as well. */
 int nq_attn_workspace_bytes(nq_attn a, int n_seqs, int n_tokens, size_t* bytes);
 /* q: [n_tokens][q_heads * head_dim] of the cache's type;  out: [n_tokens][q_heads * head_dim] of out_dtype;  lse: float [n_tokens][q_heads] or
  * NULL.  new_begin: int32 [n_seqs + 1], sequence s has the new tokens new_begin[s] .. new_begin[s + 1] - 1 (rising from 0 to n_tokens; values

@@ -14,11 +14,11 @@ struct AttnCut {
     int rows, slots, items;
     bool few;                // up to 64 rows of a sequence, on average
 };
-static AttnCut cut_attention(const nq_attn_s& a, int n_seqs, int n_tokens)
+// rows: of a sequence, on average
+static AttnCut cut_rows(const nq_attn_s& a, int64_t rows, int64_t n_seqs, int n_tokens)
 {
     AttnCut c;
     const int group = a.q_heads / a.kv.heads;
-    const int64_t rows = std::max<int64_t>(1, (int64_t)n_tokens * group / std::max(1, n_seqs));        // of a sequence, on average
     // (32 sequences of eight rows: tiles of 16 rows 130 us, of 64 137; one of 16384 rows: of 128 rows 359 us, of 64 451)
     c.few = rows <= 64;
     c.rows = rows <= 16 ? 16 : c.few || padded_dim(a.kv.head_dim) == 256 ? 64 : 128;      // (heads of 256: sums of 128 rows do not fit the registers)
@@ -27,8 +27,24 @@ static AttnCut cut_attention(const nq_attn_s& a, int n_seqs, int n_tokens)
     c.items = (int)(2 * c.slots + (int64_t)n_tokens * group / c.rows + n_seqs);
     return c;
 }
+static AttnCut cut_attention(const nq_attn_s& a, int n_seqs, int n_tokens)
+{
+    return cut_rows(a, std::max<int64_t>(1, (int64_t)n_tokens * (a.q_heads / a.kv.heads) / std::max(1, n_seqs)), n_seqs, n_tokens);
+}
 static size_t part_rows(const nq_attn_s& a, const AttnCut& c) { return (size_t)c.items * a.kv.heads * c.rows; }
-static size_t workspace_of(const nq_attn_s& a, const AttnCut& c) { return part_rows(a, c) * (padded_dim(a.kv.head_dim) + 4) * sizeof(float); }
+// Room for a call and for every call with fewer sequences or tokens, so that one buffer serves whatever batch a program has next: of the cuts that such a call may have the
+// largest (64 tokens of 32 sequences leave 16 rows to a tile, 64 of one sequence 128, with eight times the rows to an item).
+static size_t workspace_of(const nq_attn_s& a, int n_seqs, int n_tokens)
+{
+    const int64_t rows = (int64_t)n_tokens * (a.q_heads / a.kv.heads);
+    size_t most = 0;
+    for (const int least : {0, 17, 65}) {                                   // rows of a sequence, on average, from which tiles are larger
+        if (rows < least) break;
+        const int64_t seqs = least ? std::min<int64_t>(n_seqs, rows / least) : n_seqs;
+        most = std::max(most, part_rows(a, cut_rows(a, std::max(1, least), seqs, n_tokens)));
+    }
+    return most * (padded_dim(a.kv.head_dim) + 4) * sizeof(float);
+}
 
 }  // namespace nq
 
@@ -72,7 +88,7 @@ extern "C" int nq_attn_workspace_bytes(nq_attn a, int n_seqs, int n_tokens, size
     const char* const who = "nq_attn_workspace_bytes";
     if (!bytes) return refuse(NQ_E_NULL, who, "bytes is NULL");
     if (const int rc = check_sizes(who, a, n_seqs, n_tokens)) return rc;
-    *bytes = workspace_of(*a, cut_attention(*a, n_seqs, n_tokens));
+    *bytes = workspace_of(*a, n_seqs, n_tokens);
     return NQ_OK;
 }
 
@@ -96,7 +112,7 @@ extern "C" int nq_attn_forward(nq_attn a, const void* q, int64_t q_stride, const
     const AttnCut c = cut_attention(*a, n_seqs, n_tokens);
     if (!workspace) return refuse(NQ_E_NULL, who, "workspace is NULL");
     if (off_align(workspace, 16)) return refuse(NQ_E_ALIGN, who, "workspace must be 16-byte aligned");
-    if (workspace_bytes < workspace_of(*a, c)) return refuse(NQ_E_INVALID_ARG, who, "workspace too small");
+    if (workspace_bytes < workspace_of(*a, n_seqs, n_tokens)) return refuse(NQ_E_INVALID_ARG, who, "workspace too small");
     AttnArgs k = {};
     k.kv = a->kv;
     k.q = q;
