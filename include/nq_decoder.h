@@ -150,7 +150,8 @@ int nq_attn_forward(nq_attn a, const void* q, int64_t q_stride, const int32_t* n
  * -inf, or that holds a NaN, or whose temperature is negative or NaN gives token -1 and logprob NaN; +inf logits share the row among them.
  * logits: [n_rows][vocab] of dtype with row_stride elements between rows; temperature, top_p, min_p, uniform: float [n_rows]; top_k: int32
  * [n_rows]; temperature, top_k, top_p and min_p may be NULL (1, 0, 1, 0).  uniform in [0, 1).  tokens: int32 [n_rows]; logprobs: float [n_rows] or
- * NULL.  vocab <= 2^20.  workspace: 16-byte aligned, nq_sample_workspace_bytes(n_rows, vocab).  n_rows 0 does nothing. */
+ * NULL.  vocab <= 2^20.  workspace: 16-byte aligned, nq_sample_workspace_bytes(n_rows, vocab), which serves every call of fewer rows or tokens as well.
+ * n_rows 0 does nothing. */
 #define NQ_MAX_VOCAB (1 << 20)
 int nq_sample_workspace_bytes(int n_rows, int64_t vocab, size_t* bytes);
 int nq_sample(const void* logits, int dtype, int n_rows, int64_t vocab, int64_t row_stride, const float* temperature, const int32_t* top_k,

@@ -783,6 +783,19 @@ static int sample_slices(int n_rows, int64_t vocab)
     return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, vocab / 16384), kMostSlices));
 }
 
+static size_t part_bytes(int n_rows, int64_t vocab)
+{
+    const int slices = sample_slices(n_rows, vocab);
+    return slices > 1 ? (size_t)n_rows * slices * sizeof(SamplePart) : 0;
+}
+// Room for so many rows and for fewer, so that one buffer serves whatever batch a program has next: n rows have at most ceil(3 CUs / n) parts each, fewer than 3 CUs + n in all
+// (191 rows of 131071 tokens 955, 192 rows 768).
+static size_t most_part_bytes(int n_rows, int64_t vocab)
+{
+    const int64_t fill = 3 * device_cu_count(), each = std::min<int64_t>(vocab / 16384, kMostSlices), rows = std::min<int64_t>(n_rows, fill - 1);
+    return each > 1 && rows > 0 ? (size_t)std::min(each * rows, fill + rows - 1) * sizeof(SamplePart) : 0;
+}
+
 }  // namespace nq
 
 using namespace nq;
@@ -793,8 +806,7 @@ extern "C" int nq_sample_workspace_bytes(int n_rows, int64_t vocab, size_t* byte
     if (!bytes) return refuse(NQ_E_NULL, who, "bytes is NULL");
     if (n_rows < 0) return refuse(NQ_E_INVALID_ARG, who, "n_rows must be >= 0");
     if (vocab < 1 || vocab > NQ_MAX_VOCAB) return refuse(NQ_E_SHAPE, who, "vocab must be 1 to 2^20");
-    const int slices = sample_slices(n_rows, vocab);
-    *bytes = slices > 1 ? (size_t)n_rows * slices * sizeof(SamplePart) : 0;
+    *bytes = most_part_bytes(n_rows, vocab);
     return NQ_OK;
 }
 
@@ -802,8 +814,9 @@ extern "C" int nq_sample(const void* logits, int dtype, int n_rows, int64_t voca
                          const float* min_p, const float* uniform, int32_t* tokens, float* logprobs, void* workspace, size_t workspace_bytes, void* stream)
 {
     const char* const who = "nq_sample";
-    size_t need = 0;
-    if (const int rc = nq_sample_workspace_bytes(n_rows, vocab, &need)) return rc;
+    size_t most = 0;
+    if (const int rc = nq_sample_workspace_bytes(n_rows, vocab, &most)) return rc;
+    const size_t need = part_bytes(n_rows, vocab);
     if (!is_float_type(dtype)) return refuse(NQ_E_INVALID_ARG, who, "dtype must be NQ_F32, NQ_F16 or NQ_BF16");
     if (n_rows == 0) return NQ_OK;
     if (!logits || !uniform || !tokens) return refuse(NQ_E_NULL, who, "logits, uniform or tokens is NULL");

@@ -33,3 +33,19 @@ def test_attention_of_smaller_batches(hq, hk, d):
         slots = max(1, (1 if wide == 256 and rows == 16 else 2) * 256 // hk)
         assert room(seqs, tokens) >= (2 * slots + tokens * group // rows + seqs) * hk * rows * (wide + 4) * 4
     nq.nq_attn_destroy(a)
+
+
+def test_sampling_of_fewer_rows():
+    room = nq.nq_sample_workspace_bytes
+    part = 8 * 2048 + 4 * 2048 + 16                         # a part's sums, counts and the rest
+    parts = lambda n, vocab: max(1, min(-(-768 // n), vocab // 16384, 8)) * n  # noqa: E731
+    for vocab in (1000, 16384, 32000, 32768, 60000, 131071, 262144, 1 << 20):
+        sizes = [room(n, vocab) for n in range(0, 1700)]
+        assert sizes == sorted(sizes), vocab
+        for n in range(1, 1700):
+            assert sizes[n] >= (parts(n, vocab) * part if parts(n, vocab) > n else 0)
+        assert sizes[-1] <= room(1699, 1 << 20)
+    r = random.Random(2)
+    for _ in range(2000):
+        n, vocab = int(2 ** r.uniform(0, 13)), int(2 ** r.uniform(0, 20))
+        assert room(r.randint(0, n), r.randint(1, vocab)) <= room(n, vocab)
