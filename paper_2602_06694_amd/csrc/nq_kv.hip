@@ -97,8 +97,8 @@ static int same_caches(const char* who, const nq_kv* kvs, int n, KvDesc* d)
     for (int i = 1; i < n; ++i) {
         const KvDesc& e = kvs[i]->d;
         if (e.page_stride != d->page_stride || e.slot_stride != d->slot_stride || e.head_stride != d->head_stride || e.n_pages != d->n_pages ||
-            e.heads != d->heads || e.head_dim != d->head_dim || e.page_shift != d->page_shift)
-            return refuse(NQ_E_INVALID_ARG, who, "the caches differ in shape or strides");
+            e.heads != d->heads || e.head_dim != d->head_dim || e.page_shift != d->page_shift || e.dtype != d->dtype)
+            return refuse(NQ_E_INVALID_ARG, who, "the caches differ in shape, strides or type");
     }
     return NQ_OK;
 }
