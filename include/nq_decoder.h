@@ -126,7 +126,8 @@ int nq_rope_backward(nq_rope r, const void* q, int64_t q_stride, const void* k, 
  * 8 bits of an NQ_BF16 cache, 11 of an NQ_F16 one: the results are then about as far from binary64 again as their own rounding leaves them (2-norm: 2.3e-3 instead of 1.7e-3
  * for NQ_BF16).  Who wants those finer asks for NQ_F32 results. */
 
-/* out_dtype: of the results; q has the cache's type.  Copies what it needs of kv (which may be destroyed).  q_heads a multiple of the cache's kv_heads.  Host only. */
+/* out_dtype: of the results; q has the cache's type.  Copies what it needs of kv (which may be destroyed).  q_heads a multiple of the cache's kv_heads.
+ * scale finite, cap 0 or above; scale, cap and scale / cap have to be numbers of fp32 (about 1e-38 to 2e38).  Host only. */
 int nq_attn_create(nq_attn* out, nq_kv kv, int q_heads, double scale, double cap, int out_dtype);
 int nq_attn_destroy(nq_attn a);
 /* Workspace of a call with n_seqs sequences and n_tokens new tokens in all; it serves every call with fewer of either as well. */

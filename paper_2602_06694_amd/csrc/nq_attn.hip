@@ -58,6 +58,11 @@ extern "C" int nq_attn_create(nq_attn* out, nq_kv kv, int q_heads, double scale,
     if (!kv) return refuse(NQ_E_NULL, who, "NULL cache");
     if (q_heads < 1 || q_heads % kv->d.heads || q_heads > 65535) return refuse(NQ_E_SHAPE, who, "q_heads must be a multiple of the cache's heads, at most 65535");
     if (!std::isfinite(scale) || !std::isfinite(cap) || cap < 0.0) return refuse(NQ_E_INVALID_ARG, who, "scale must be finite, cap finite and >= 0");
+    // what the kernels form of them in 32 bits: scale log2(e), cap log2(e), scale / cap
+    const double most = 2.3e38, least = 1.2e-38, slope = std::fabs(scale) / cap;
+    if (std::fabs(scale) > most) return refuse(NQ_E_INVALID_ARG, who, "scale is beyond fp32");
+    if (cap > 0.0 && (cap < least || cap > most || (scale != 0.0 && (slope < least || slope > most))))
+        return refuse(NQ_E_INVALID_ARG, who, "cap, or scale / cap, is beyond fp32");
     if (!is_float_type(out_dtype)) return refuse(NQ_E_INVALID_ARG, who, "out_dtype must be NQ_F32, NQ_F16 or NQ_BF16");
     nq_attn a = new (std::nothrow) nq_attn_s{kv->d, q_heads, out_dtype, (float)scale, (float)cap};
     if (!a) return refuse(NQ_E_HIP, who, "out of host memory");

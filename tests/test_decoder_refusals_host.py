@@ -15,3 +15,20 @@ def test_caches_of_different_types_are_not_moved_together():
     assert nq.lib().nq_kv_compact(both, 2, A, A, 4, A, 4, A, 0, None) == nq.NQ_E_INVALID_ARG
     for h in (a, b):
         nq.nq_kv_destroy(h)
+
+
+@pytest.mark.parametrize("scale,cap", [(1e39, 0.0), (-1e300, 0.0), (3e38, 0.0), (1.0, 1e-50), (1.0, 1e-39), (1.0, 1e39), (1.0, 3e38), (1.0, 1e300), (1e10, 1e-30), (1e-3, 1e38), (1e-60, 1.0)])
+def test_scales_and_caps_that_fp32_does_not_hold(scale, cap):
+    """A cap that rounds to zero would be none, one beyond fp32 would make NaN of all scores."""
+    kv = nq.nq_kv_create(A, A, nq.NQ_BF16, 2, 64, 16, 8)
+    with pytest.raises(nq.NQError) as e:
+        nq.nq_attn_create(kv, 4, scale, cap, nq.NQ_F32)
+    assert e.value.status == nq.NQ_E_INVALID_ARG
+    nq.nq_kv_destroy(kv)
+
+
+@pytest.mark.parametrize("scale,cap", [(1.0, 0.0), (0.0, 0.0), (-0.125, 0.0), (0.0, 30.0), (-0.125, 30.0), (0.125, 1e30), (0.125, 1e-30), (1e-60, 0.0), (2e38, 0.0)])
+def test_scales_and_caps_that_are_taken(scale, cap):
+    kv = nq.nq_kv_create(A, A, nq.NQ_BF16, 2, 64, 16, 8)
+    nq.nq_attn_destroy(nq.nq_attn_create(kv, 4, scale, cap, nq.NQ_F32))
+    nq.nq_kv_destroy(kv)
