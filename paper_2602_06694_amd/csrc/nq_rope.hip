@@ -554,8 +554,8 @@ extern "C" int nq_rope_create(nq_rope* out, int q_heads, int kv_heads, int head_
     if (rot_dim > 0 && !inv_freq) return refuse(NQ_E_NULL, who, "inv_freq is NULL");
     for (int i = 0; i < rot_dim / 2; ++i)
         if (!std::isfinite(inv_freq[i])) return refuse(NQ_E_INVALID_ARG, who, "inv_freq holds a value that is not finite");
-    if (!std::isfinite(magnitude) || !std::isfinite(weight_offset)) return refuse(NQ_E_INVALID_ARG, who, "magnitude and weight_offset must be finite");
-    if (!(eps >= 0.0) || !std::isfinite(eps)) return refuse(NQ_E_INVALID_ARG, who, "eps must be at least 0");
+    if (!std::isfinite((float)magnitude) || !std::isfinite((float)weight_offset)) return refuse(NQ_E_INVALID_ARG, who, "magnitude and weight_offset must be finite in fp32");
+    if (!(eps >= 0.0) || !std::isfinite((float)eps)) return refuse(NQ_E_INVALID_ARG, who, "eps must be at least 0 and finite in fp32");
     if (!is_float_type(in_dtype) || !is_float_type(out_dtype)) return refuse(NQ_E_INVALID_ARG, who, "types must be NQ_F32, NQ_F16 or NQ_BF16");
     int device = -1;
     NQ_HIP(hipGetDevice(&device));

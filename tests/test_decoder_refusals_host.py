@@ -32,3 +32,13 @@ def test_scales_and_caps_that_are_taken(scale, cap):
     kv = nq.nq_kv_create(A, A, nq.NQ_BF16, 2, 64, 16, 8)
     nq.nq_attn_destroy(nq.nq_attn_create(kv, 4, scale, cap, nq.NQ_F32))
     nq.nq_kv_destroy(kv)
+
+
+@pytest.mark.parametrize("change", [dict(magnitude=1e39), dict(magnitude=-1e300), dict(eps=1e39), dict(weight_offset=1e60), dict(weight_offset=-4e38)])
+def test_rotations_of_numbers_that_fp32_does_not_hold(change):
+    """They are held in 32 bits: what is finite in binary64 alone would be an infinity there."""
+    a = dict(q_heads=4, kv_heads=2, head_dim=64, rot_dim=0, layout=nq.NQ_ROPE_HALF, inv_freq=None, magnitude=1.0, eps=1e-6, weight_offset=0.0, in_dtype=nq.NQ_F32,
+             out_dtype=nq.NQ_BF16)
+    with pytest.raises(nq.NQError) as e:
+        nq.nq_rope_create(**{**a, **change})
+    assert e.value.status == nq.NQ_E_INVALID_ARG
