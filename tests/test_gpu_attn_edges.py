@@ -129,3 +129,27 @@ def test_an_infinite_value_of_a_small_weight(dtype, new, d):
     assert bool((out[..., 5] == math.inf).all()) and bool((out[..., 9] == -math.inf).all())
     assert int((~torch.isfinite(out)).sum()) == 2 * new * 4 and bool(torch.isfinite(lse).all())
     p.done()
+
+
+@pytest.mark.parametrize("new,out", [(10, "bf16"), (20, "f32"), (20, "bf16")])
+def test_many_sequences_of_many_rows(new, out):
+    """More than a wave looks at in one go, through tiles of 64 and of 128 rows; some have no tokens."""
+    g = torch.Generator()
+    g.manual_seed(9)
+    ctx = torch.randint(0, 150, (140,), generator=g).tolist()
+    p = Problem(101, ctx, [0 if i % 13 == 4 else new + i % 3 for i in range(140)], 4, 1, 64, "bf16", out)
+    got, lse = p.run()
+    p.check(got, lse)
+    p.done()
+
+
+@pytest.mark.parametrize("dtype,out", [("f16", "f16"), ("f16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("new,cap", [(1, 0.0), (10, 0.0), (60, 0.0), (60, 15.0)])
+def test_negative_scales(dtype, out, new, cap):
+    """Minus the scale is minus the queries (not to the bit: sums of the matrix instructions are not rounded alike for both signs)."""
+    p = Problem(111, [300], [new], 4, 1, 64, dtype, out, cap=cap)
+    p.scale, p.q = -p.scale, -p.q
+    got, lse = p.run()
+    p.scale, p.q = -p.scale, -p.q
+    p.check(got, lse)
+    p.done()
