@@ -178,6 +178,12 @@ class Server:
             at = len(nodes) - 1
         return nodes
 
+    @staticmethod
+    def _pack(rows, nodes):
+        """Whole numbers whose bit j says that a node sees node j, as words of 32 bits: [rows, words]."""
+        words = np.array([[row >> 32 * w & 0xffffffff for w in range(-(-nodes // 32))] for row in rows], dtype=np.uint32)
+        return torch.from_numpy(words.view(np.int32))
+
     def step(self, seqs, temperature, top_k, top_p, min_p, uniforms, most=6):
         """Advances every sequence by at least one token; returns how many each gained.  uniforms: a number per sequence and depth."""
         drafts = [self._draft(s, most) for s in seqs]
@@ -189,7 +195,7 @@ class Server:
                 see.append((see[parent] if parent >= 0 else 0) | 1 << j)
             depths.append(depth)
             rows += see
-        logits = self._run(seqs, [[t for t, _ in nodes] for nodes in drafts], depths, self._ints(rows).view(-1, 1))
+        logits = self._run(seqs, [[t for t, _ in nodes] for nodes in drafts], depths, self._pack(rows, max(len(nodes) for nodes in drafts)).cuda())
         n = len(rows)
         own = [i for i, nodes in enumerate(drafts) for _ in nodes]
         per = lambda values, dtype: torch.tensor([values[i] for i in own], dtype=dtype, device="cuda")  # noqa: E731
