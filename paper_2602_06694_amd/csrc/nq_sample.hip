@@ -48,6 +48,10 @@ struct SamplePart {
     int nan;
 };
 
+struct TopLds {                                     // of the waves
+    float top[kSampleThreads / 64];
+    int nan[kSampleThreads / 64];
+};
 struct SampleLds {
     uint64_t mass[kBins], mass2[kBins];             // running sums over the bins; of the bins a crowded bin is cut into
     uint32_t count[kBins], count2[kBins];           // count: where top-k asks for it exactly, else bounds from above
@@ -55,8 +59,7 @@ struct SampleLds {
     uint32_t rank[kListed], weight[kListed];
     uint64_t part_mass[16], lo, hi;
     uint32_t part_count[16], n, found;
-    float part_top[16];
-    int part_nan[16];
+    TopLds part_top;
 };
 
 // x's place in falling order, then the token: ascending numbers are the order of the tokens
@@ -484,9 +487,9 @@ __device__ __forceinline__ Answer locate(SampleLds& s, Row& r, const Question& a
     return a;
 }
 
-// the largest logit of a span, and whether one is NaN, to all threads; the bins are cleared on the way
+// the largest logit of a span, and whether one is NaN, to all threads
 template <int DT>
-__device__ __forceinline__ void span_top(SampleLds& s, const void* logits, const Span& span, float* top_out, int* nan_out)
+__device__ __forceinline__ void span_top(TopLds& s, const void* logits, const Span& span, float* top_out, int* nan_out)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     float top;
@@ -507,12 +510,11 @@ __device__ __forceinline__ void span_top(SampleLds& s, const void* logits, const
         top = fmaxf(top, __shfl_xor(top, m));
         nan |= __shfl_xor(nan, m);
     }
-    if (lane == 0) { s.part_top[wave] = top; s.part_nan[wave] = nan; }
-    for (int b = threadIdx.x; b < kBins; b += kSampleThreads) { s.count[b] = 0; s.mass[b] = 0; }
+    if (lane == 0) { s.top[wave] = top; s.nan[wave] = nan; }
     __syncthreads();
     for (int w = 0; w < kSampleThreads / 64; ++w) {
-        top = fmaxf(top, s.part_top[w]);
-        nan |= s.part_nan[w];
+        top = fmaxf(top, s.top[w]);
+        nan |= s.nan[w];
     }
     *top_out = top;
     *nan_out = nan;
@@ -597,8 +599,7 @@ __device__ __forceinline__ void span_counts(SampleLds& s, const void* logits, co
 template <int DT>
 __global__ __launch_bounds__(kSampleThreads, 8) void sample_top_kernel(SampleArgs a)
 {
-    extern __shared__ char lds[];
-    SampleLds& s = *(SampleLds*)lds;
+    __shared__ TopLds s;
     float top;
     int nan;
     span_top<DT>(s, (const char*)a.logits + blockIdx.y * a.row_stride * (DT == NQ_F32 ? 4 : 2), Span(a.vocab, blockIdx.x, a.slices), &top, &nan);
@@ -653,7 +654,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a)
     float top;
     int nan;
     if (a.slices == 1) {
-        span_top<DT>(s, r.logits, Span(a.vocab, 0, 1), &top, &nan);
+        for (int b = threadIdx.x; b < kBins; b += kSampleThreads) { s.count[b] = 0; s.mass[b] = 0; }       // (before the barrier in span_top)
+        span_top<DT>(s.part_top, r.logits, Span(a.vocab, 0, 1), &top, &nan);
     } else {
         parts_top(a, row, &top, &nan);
     }
@@ -832,22 +834,13 @@ extern "C" int nq_sample(const void* logits, int dtype, int n_rows, int64_t voca
     auto launch = [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         const dim3 block(kSampleThreads);
-        if (a.slices > 1) {
-            NQ_ALLOW_LDS((sample_top_kernel<DT>), sizeof(SampleLds));
+        if (a.slices > 1) {                                              // (fewer rows than three to a CU)
             NQ_ALLOW_LDS((sample_bins_kernel<DT>), sizeof(SampleLds));
-            for (int r0 = 0; r0 < n_rows; r0 += 65535) {                 // (rows are the grid's second dimension)
-                SampleArgs part = a;
-                const int rows = std::min(65535, n_rows - r0);
-                part.logits = (const char*)logits + (int64_t)r0 * row_stride * type_bytes(dtype);
-                part.parts = a.parts + (int64_t)r0 * a.slices;
-                if (temperature) part.temperature += r0;
-                if (top_k) part.top_k += r0;
-                if (min_p) part.min_p += r0;
-                hipLaunchKernelGGL((sample_top_kernel<DT>), dim3(a.slices, rows), block, sizeof(SampleLds), (hipStream_t)stream, part);
-                if (const int rc = launched(who)) return rc;
-                hipLaunchKernelGGL((sample_bins_kernel<DT>), dim3(a.slices, rows), block, sizeof(SampleLds), (hipStream_t)stream, part);
-                if (const int rc = launched(who)) return rc;
-            }
+            const dim3 grid(a.slices, n_rows);
+            hipLaunchKernelGGL((sample_top_kernel<DT>), grid, block, 0, (hipStream_t)stream, a);
+            if (const int rc = launched(who)) return rc;
+            hipLaunchKernelGGL((sample_bins_kernel<DT>), grid, block, sizeof(SampleLds), (hipStream_t)stream, a);
+            if (const int rc = launched(who)) return rc;
         }
         NQ_ALLOW_LDS((sample_kernel<DT>), sizeof(SampleLds));
         hipLaunchKernelGGL((sample_kernel<DT>), dim3(n_rows), block, sizeof(SampleLds), (hipStream_t)stream, a);
