@@ -568,11 +568,11 @@ def nq_kv_create(k, v, dtype: int, kv_heads: int, head_dim: int, page_size: int,
     """k, v: device tensors (or addresses) that hold the pages; strides in elements, 0, 0, 0: [n_pages][kv_heads][page_size][head_dim], for which tensors have to be
     contiguous.  Tensors have to hold all pages."""
     h = ctypes.c_void_p()
-    at, tensors = [], []
+    kind, at, tensors = _torch_type(dtype), [], []
     for t in (k, v):
         if t is not None and not isinstance(t, int):
-            if t.dtype != _torch_type(dtype):
-                raise ValueError(f"k, v: expected {_torch_type(dtype)}, got {t.dtype}")
+            if t.dtype != kind:
+                raise ValueError(f"k, v: expected {kind}, got {t.dtype}")
             if not t.is_cuda:
                 raise ValueError("k, v: expected device (cuda) tensors")
             tensors.append(t)
@@ -587,7 +587,7 @@ def nq_kv_create(k, v, dtype: int, kv_heads: int, head_dim: int, page_size: int,
         if need > (t.numel() if whole else _extent(t)) or (packed and not whole):
             lib().nq_kv_destroy(h)
             raise ValueError(f"k, v: the pages take {need} elements, {tuple(t.shape)} of strides {t.stride()} are no room for them")
-    _WIDTHS[h.value] = (head_dim, _torch_type(dtype))
+    _WIDTHS[h.value] = (head_dim, kind)
     return h.value
 
 
