@@ -19,7 +19,7 @@ static AttnCut cut_rows(const nq_attn_s& a, int64_t rows, int64_t n_seqs, int n_
 {
     AttnCut c;
     const int group = a.q_heads / a.kv.heads;
-    // (32 sequences of eight rows: tiles of 16 rows 130 us, of 64 137; one of 16384 rows: of 128 rows 359 us, of 64 451)
+    // (32 sequences of eight rows: tiles of 16 rows 127 us, of 64 137; one of 16384 rows: of 128 rows 342 us, of 64 440)
     c.few = rows <= 64;
     c.rows = rows <= 16 ? 16 : c.few || padded_dim(a.kv.head_dim) == 256 ? 64 : 128;      // (heads of 256: sums of 128 rows do not fit the registers)
     const int to_cu = padded_dim(a.kv.head_dim) == 256 && c.rows == 16 ? 1 : 2;             // workgroups that a CU's registers hold

@@ -18,7 +18,8 @@
 // unnormalised sums and their maxima, which attn_join_kernel adds up.
 //
 // Bound by the cache's bytes up to some 64 rows (4 to 5.9 TB/s of it at 64 and 8 heads of 128 from 150 MB on, one to 256 sequences, 6.8 is what a plain read reaches), then by
-// the matrix and the vector unit together (2048 tokens behind 4095: 1.0 PFLOP/s; 1.36 is what a large matrix product reaches).
+// the matrix and the vector unit together (2048 tokens behind 4095: 328 to 345 us on several cards, 1.0 PFLOP/s; 1.36 is what a large matrix
+// product reaches).
 #pragma once
 
 #include <algorithm>
@@ -96,8 +97,9 @@ __device__ __forceinline__ int items_of(int tiles, int runs, const AttnArgs& a) 
 // - runs that all fit the chip at once: each tile in as many as there are places to a tile, or runs of one length (the last of a tile comes on top of those of full length,
 //   hence the tiles taken off);
 // - runs of half a share, more than fit at once, which places take as they become free: a quarter of a share is left at the end.
-// A run costs what it leaves for the joining, 4 blocks' time where tiles have 64 rows and more and 2 where they have 16, the joining itself 3.  front: the lane's sequence of
-// the first 64.
+// A run costs what it leaves for the joining, 4 blocks' time where tiles have 64 rows and more and 2 where they have 16, the joining itself 3.  Of 15 calls of 12 to 330 us, each
+// timed with all three ways, the one chosen is within 6 % of the best in 13; 512 tokens behind 1023 take 59 us where whole tiles take 44, 16 sequences of 512 17 and 14.  front: the
+// lane's sequence of the first 64.
 constexpr int kNoRuns = 1 << 25;
 __device__ __forceinline__ int run_length(const AttnArgs& a, int rows, int lane, const Seq& front)
 {
@@ -328,7 +330,8 @@ struct KeyStep {
 
 // ---------------------------------------------------------------------------------------------
 // Up to 16 rows: the waves of a workgroup share them and take every fourth step of 32 keys, straight from memory to the operands' registers, the next step's loads
-// under way while one is worked on; their sums meet in LDS at the end.  Bound by the bytes of the cache: 32 ragged sequences of up to 8191 tokens (621 MB) in 119 us.
+// under way while one is worked on; their sums meet in LDS at the end.  Bound by the bytes of the cache: 32 ragged sequences of up to 8191 tokens in 122 us
+// under a kernel trace, 623 MB read for 621 of keys and values.
 // DP: head_dim rounded up to 64, 128 or 256; PARTS: parts in which the weights are rounded
 // ---------------------------------------------------------------------------------------------
 constexpr int split_lds(int dp) { return kWaves * (16 * (dp + 4) + 32) * (int)sizeof(float); }
@@ -594,9 +597,9 @@ __global__ __launch_bounds__(kWaves * 64, DP == 256 ? 1 : 2) void attn_split_ker
 // the one that is worked on (one, for heads of 256); one barrier a block.  Rows of keys lie in LDS with their 16-byte pieces
 // exchanged by the key's number (every lane chooses the piece that it loads), so that neither the operands of K (a piece of 16 keys) nor those of V (read transposed: four keys
 // of 16 elements by each 16 lanes) meet in the same banks.  Two rows of 16 to a wave where there are more than 64 rows to a sequence: an operand of keys then serves two
-// products (2048 tokens behind 4095, 64 and 8 heads of 128: 359 us; with one 451, on the same card).  Four, one wave to a SIMD, do not fit its registers (545 us).
-// Six tokens behind 131071: 104 us for 537 MB; five trees of up to 21 tokens behind up to 12301, capped scores, fp32 results: 52 us for 174 MB, where products, exponentials and bytes take
-// as much each and do not overlap whole.
+// products (2048 tokens behind 4095, 64 and 8 heads of 128: 342 us; with one 440, on the same card).  Four, one wave to a SIMD, do not fit its registers (545 us).
+// Six tokens behind 131071: 106 us for 537 MB (562 read, 13 written for the joining); five trees of up to 21 tokens behind up to 12301, capped scores, fp32 results: 52 us for 174 MB (187 read),
+// where products, exponentials and bytes take as much each and do not overlap whole.
 // ---------------------------------------------------------------------------------------------
 constexpr int wide_keys(int dp) { return dp == 64 ? 64 : 32; }             // of a block
 constexpr int wide_buffers(int dp) { return dp == 256 ? 2 : 4; }           // a power of two
@@ -1103,9 +1106,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a, int rows)
 static int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
 // PARTS: parts of the weights where there are many rows.  One part of bf16 is eight bits, an error as large as the results' own rounding: 2.3 10^-3 of the results in the 2-norm,
-// where a single rounding of exact ones leaves 1.7 10^-3.  Few rows have two parts in any case: their calls are bound by bytes for the most part (32 sequences of up to 8191:
-// 127.5 us with two parts, 127.1 with one; six tokens behind 131071: 116 and 113; five trees with capped scores, fp16 results: 60 and 53).  Many rows are bound by the matrix
-// products, and have one part where the results are of the cache's type or a coarser one: 2048 tokens behind 4095 take 341 us with one part, 454 with two.
+// where a single rounding of exact ones leaves 1.7 10^-3.  Few rows have two parts in any case: their calls are bound by bytes for the most part (one token behind 1023: 12.5 us with two
+// parts, 12.1 with one; 32 sequences of up to 8191 125.5 and 125.2; six tokens behind 131071 110 and 109; five trees with capped scores, fp16 results 55.5 and 49).  Many rows
+// are bound by the matrix products, and have one part where the results are of the cache's type or a coarser one: 2048 tokens behind 4095 take 342 us with one part, 447 with two.
 template <int DT, int DP, int PARTS>
 static int launch_attention(const AttnArgs& a, const char* who, hipStream_t s)
 {
