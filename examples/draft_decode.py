@@ -158,7 +158,8 @@ class Server:
 
     def prefill(self, seq, tokens):
         """All but the last token of a prompt; the last one is the root of the first step."""
-        self._run([seq], [tokens[:-1]], [range(len(tokens) - 1)], None)
+        if len(tokens) > 1:
+            self._run([seq], [tokens[:-1]], [range(len(tokens) - 1)], None)
         seq["length"], seq["tokens"] = len(tokens) - 1, list(tokens)
         for a, b in zip(tokens, tokens[1:]):
             seq["follows"].setdefault(a, []).append(b)

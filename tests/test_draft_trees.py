@@ -26,3 +26,12 @@ def test_many_drafts_do_not_change_the_tokens():
     many, few = (draft_decode.generate(model, prompt, 30, greedy=True, drafts=d) for d in (40, 0))
     model.close()
     assert many[:2] == few[:2]
+
+
+@pytest.mark.gpu
+def test_a_prompt_of_one_token():
+    import draft_decode
+    model = draft_decode.Model(vocab=60)
+    many, few = (draft_decode.generate(model, [7], 12, greedy=True, drafts=d) for d in (5, 0))
+    model.close()
+    assert many[:2] == few[:2] and len(few[0]) == 12
