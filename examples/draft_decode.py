@@ -100,7 +100,7 @@ class Server:
 
     def fork(self, seq):
         """A second sequence behind the same tokens: full pages are shared, a partly filled one is copied."""
-        other = {"pages": list(seq["pages"]), "length": seq["length"], "tokens": list(seq["tokens"]), "follows": dict(seq["follows"])}
+        other = {"pages": list(seq["pages"]), "length": seq["length"], "tokens": list(seq["tokens"]), "follows": {t: list(n) for t, n in seq["follows"].items()}}
         for p in other["pages"]:
             self.users[p] += 1
         if other["length"] % self.page:

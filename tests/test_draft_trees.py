@@ -35,3 +35,15 @@ def test_a_prompt_of_one_token():
     many, few = (draft_decode.generate(model, [7], 12, greedy=True, drafts=d) for d in (5, 0))
     model.close()
     assert many[:2] == few[:2] and len(few[0]) == 12
+
+
+def test_a_fork_drafts_from_its_own_tokens():
+    from types import SimpleNamespace
+
+    import draft_decode
+    seq = {"pages": [0], "length": 16, "tokens": list(range(17)), "follows": {3: [4]}}
+    other = draft_decode.Server.fork(SimpleNamespace(users=[1], page=16), seq)
+    other["follows"][3].append(9)
+    other["pages"].append(1)
+    other["tokens"].append(5)
+    assert seq["follows"] == {3: [4]} and seq["pages"] == [0] and len(seq["tokens"]) == 17
