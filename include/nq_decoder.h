@@ -134,7 +134,7 @@ int nq_attn_destroy(nq_attn a);
 int nq_attn_workspace_bytes(nq_attn a, int n_seqs, int n_tokens, size_t* bytes);
 /* q: [n_tokens][q_heads * head_dim] of the cache's type;  out: [n_tokens][q_heads * head_dim] of out_dtype;  lse: float [n_tokens][q_heads] or
  * NULL.  new_begin: int32 [n_seqs + 1], sequence s has the new tokens new_begin[s] .. new_begin[s + 1] - 1 (rising from 0 to n_tokens; values
- * beyond are cut).  ctx_len: int32 [n_seqs].  page_table: int32 [n_seqs][table_stride]; tokens beyond the table are not seen, a page outside the cache is
+ * beyond are cut, and where it does not rise rows may be left unwritten).  ctx_len: int32 [n_seqs].  page_table: int32 [n_seqs][table_stride]; tokens beyond the table are not seen, a page outside the cache is
  * read as one inside it.  tree: [n_tokens][tree_words] or NULL.  workspace: 16-byte aligned.  n_tokens 0 does nothing. */
 int nq_attn_forward(nq_attn a, const void* q, int64_t q_stride, const int32_t* new_begin, const int32_t* ctx_len, const int32_t* page_table,
                     int64_t table_stride, const uint32_t* tree, int tree_words, int n_seqs, int n_tokens, void* out, int64_t out_stride, float* lse,
