@@ -18,7 +18,7 @@
 // unnormalised sums and their maxima, which attn_join_kernel adds up.
 //
 // Bound by the cache's bytes up to some 64 rows (4 to 5.9 TB/s of it at 64 and 8 heads of 128 from 150 MB on, one to 256 sequences, 6.8 is what a plain read reaches), then by
-// the matrix and the vector unit together (2048 tokens behind 4095: 328 to 345 us on several cards, 1.0 PFLOP/s; 1.36 is what a large matrix
+// the matrix and the vector unit together (2048 tokens behind 4095: 323 to 345 us on several cards, 1.0 PFLOP/s; 1.36 is what a large matrix
 // product reaches).
 #pragma once
 
